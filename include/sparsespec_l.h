@@ -602,7 +602,9 @@ int ssl_cache_append(const ssl_coded_cache *cache, int32_t n_kv_heads, int32_t n
  * finite there) and probabilities are fp32; the value product uses the probabilities
  * times V's scale, rounded to fp16 relative to their row's largest (11 bits; below
  * 2^-31 of it they lose bits, then count as 0), and the codes, which fp16 holds
- * exactly; V's scales must be at most 2^110, and values below 2^-90 may count as 0.
+ * exactly.  V's scales may be any that the append writes, or that are finite and
+ * >= 0; values below 2^-90 may count as 0, and an output element that passes fp32's
+ * range is an infinity, the row's others as they are.
  * block_table as there (entries are clamped into the pool); rows of a sequence's last
  * page past its length are never used.  Codes must not be NaN (the append writes none).
  * params->verify_mode:

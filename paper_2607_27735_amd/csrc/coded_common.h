@@ -86,18 +86,84 @@ __device__ __forceinline__ void decode_pairs_f16(uint32_t x, uint32_t y, uint32_
     }
 }
 
-// Probabilities for a value product in fp16.  A key's probability is held as p =
-// 2^(y - M) and its weight, p times its V scale s, is what is rounded: fp16 gives
-// it 11 bits, where bf16 would give 8 (a single bf16 rounding of the weights is
-// as large as the output's own).  So that the weights keep within fp16's range
-// whatever the scales, the reference M follows the row's maximum of y + e, e the
-// exponent of s: it is set kBelow under that maximum and moves when a weight
-// would pass 2^(kAbove + 1).  Weights then span 2^-24 (2^-31 of the largest) to
-// 2^16.  M is whole, so moving it is exact.  e is kept within bounds that leave
-// p and its sum room in fp32.
+// A row's probabilities and the weights of its value product.  A key's probability
+// is held as p = 2^(y - M), M near the row's maximum of y: its sum and the scores
+// come from it and do not depend on V.  Its weight, 2^y times its V scale s = 2^e r,
+// is rounded to fp16, which gives it 11 bits, where bf16 would give 8 (a single bf16
+// rounding of the weights is as large as the output's own).  So that weights keep
+// within fp16's range whatever the scales, they are relative to a reference of
+// their own, N, which follows the row's maximum of y + e: w = 2^(y + e - N) r.  (One
+// reference for both would put p out of fp32's range where scales are far apart.)
+// A reference is set kBelow under its maximum and moves when a key passes it by
+// kAbove.  Weights then span 2^-24 (2^-31 of the largest) to 2^15.  References are
+// whole numbers, so that moving them is exact.
 constexpr float kBelow = 7.f, kAbove = 14.f;
-__device__ __forceinline__ float v_exponent(float s) {
-    return (float)min(max((int)(__float_as_uint(s) >> 23) - 127, -90), 110);
+constexpr float kNoRef = -3.402823466e38f;   // reference of a row without keys so far
+// A partial output is relative to M, as its sum is, and held 2^-kPartialExp times:
+// so a row's whole sum passes fp32's range only where its output is about to, and
+// values down to 2^-90 keep their bits.
+constexpr int kPartialExp = 36;
+constexpr float kWhole = 0x1p36f;
+
+// x >= 0 as 2^exponent(x) rest(x), rest(x) below 2
+__device__ __forceinline__ float exponent(float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); }
+__device__ __forceinline__ float rest(float x) { return __builtin_ldexpf(x, 127 - (int)(__float_as_uint(x) >> 23)); }
+
+// The exponent that takes a wave's sum of w code (relative to M + D) to its share of
+// the partial output relative to Mx.  Not a factor: D may lie past fp32's range.
+__device__ __forceinline__ int partial_shift(float M, float D, float Mx) {
+    return (int)fmaxf(M - Mx + D, -300.f) - kPartialExp;
+}
+__device__ __forceinline__ f32x4 times_2(f32x4 o, int shift) {
+    return f32x4{__builtin_ldexpf(o[0], shift), __builtin_ldexpf(o[1], shift), __builtin_ldexpf(o[2], shift),
+                 __builtin_ldexpf(o[3], shift)};
+}
+
+// p and w of the lane's eight keys of a tile for one row (y not yet scaled, masked
+// keys -inf); D = N - M; more_p and more_o rescale what the row has summed.
+template <typename MoreP, typename MoreO>
+__device__ __forceinline__ void key_weights(const f32x4 (&y)[2], float scale, float ve, float vr, float& M, float& D, float& L,
+                                            f32x4 (&p)[2], f32x4 (&w)[2], MoreP&& more_p, MoreO&& more_o) {
+    constexpr float kFar = 100.f;   // 2^shift that a probability and its factor still hold together
+    float mx = y[0][0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, y[e >> 2][e & 3]);
+    const float over = __builtin_fmaf(mx, scale, -M);
+    float shift = ve - D;   // w = p 2^shift vr
+    bool far = false;
+    if (__any(fmaxf(fmaxf(over, over + shift), shift - (kFar - kAbove)) > kAbove)) {
+        // the wave's first tile, a key far above a reference, or scales far apart
+        mx = fmaxf(mx, shfl_xor_f(mx, 16));
+        mx = fmaxf(mx, shfl_xor_f(mx, 32)) * scale;
+        const float N = M + D;
+        const bool grow = mx > M + kAbove, grow_o = mx + ve > N + kAbove;
+        const float Mn = grow ? ceilf(mx) - kBelow : M, Nn = grow_o ? ceilf(mx + ve) - kBelow : N;
+        if (__any(grow && M != kNoRef)) {
+            const float alpha = fast_exp2(M - Mn);   // (1 where it stays)
+            L *= alpha;
+            more_p(alpha, grow && M != kNoRef);
+        }
+        if (__any(grow_o && M != kNoRef)) more_o(fast_exp2(N - Nn));
+        M = Mn;
+        D = Nn - Mn;
+        shift = ve - D;
+        far = __any(shift > kFar);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        p[e >> 2][e & 3] = fast_exp2(__builtin_fmaf(y[e >> 2][e & 3], scale, -M));
+        sum += p[e >> 2][e & 3];
+    }
+    L += sum;
+    const float c = __builtin_ldexpf(vr, (int)shift);
+    w[0] = p[0] * c;
+    w[1] = p[1] * c;
+    if (far) {   // (wave-uniform) a probability that fp32 does not hold may still count
+        const float at = shift - M;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e >> 2][e & 3] = fast_exp2(__builtin_fmaf(y[e >> 2][e & 3], scale, at)) * vr;
+    }
 }
 
 // A 32-key tile of codes in registers.
@@ -148,7 +214,7 @@ __device__ __forceinline__ void decode_v(const u32x2 (&v)[8], int h, u32x4 (&a)[
 // Page ids outside the pool are clamped into it.
 struct TileRun {
     uint32_t off_lo, off_hi;   // byte offset of the tile in the pool of codes
-    float ks, vs;              // its scales (a scale block holds whole tiles)
+    float ks, ve, vr;          // its scales, V's as 2^ve vr (a scale block holds whole tiles)
     int first;
 };
 
@@ -166,7 +232,9 @@ __device__ __forceinline__ TileRun tile_run(const CodedKV& c, const int32_t* tab
     r.off_lo = (uint32_t)off;
     r.off_hi = (uint32_t)(off >> 32);
     r.ks = c.k_scale[at];
-    r.vs = c.v_scale[at];
+    const float vs = c.v_scale[at];
+    r.ve = exponent(vs);
+    r.vr = rest(vs);
     return r;
 }
 

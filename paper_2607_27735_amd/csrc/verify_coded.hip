@@ -9,7 +9,7 @@
 //
 //   coded_sweep_kernel   reads K and V once: per item (sequence, KV head, key
 //                        chunk) and row the running maximum and sum of 2^y and
-//                        the partial sum of P V relative to that maximum;
+//                        the partial output over the item's keys;
 //   coded_finish_kernel  its first workgroups read K again and write the
 //                        scores 2^(y - lse); the others add the items' partial
 //                        outputs, one row each.
@@ -34,7 +34,7 @@ namespace {
 using namespace vc;
 using namespace cc;
 
-constexpr float kEmpty = -3.402823466e38f;   // reference maximum of a row without keys so far
+constexpr float kEmpty = kNoRef;
 
 // decode_item() without its chain of loads: sixteen starts are compared at a
 // time (those past the last sequence are larger than any item).
@@ -89,12 +89,12 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
 
     u32x4 q[NRT];
     q_load<NRT>(a, it.b, it.c, it.nq, it.qoff, q);
-    float M[NRT], L[NRT];
+    float M[NRT], D[NRT], L[NRT];
     f32x4 oacc[8][NRT];
 #pragma unroll
     for (int rt = 0; rt < NRT; ++rt) {
         M[rt] = kEmpty;
-        L[rt] = 0.f;
+        D[rt] = L[rt] = 0.f;
 #pragma unroll
         for (int jd = 0; jd < 8; ++jd) oacc[jd][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -127,36 +127,20 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
             }
         }
     };
-    // The keys' weights (see v_exponent) in fp16.
-    auto probs = [&](const f32x4 (&y)[NRT][2], float ks, float vs, u32x4 (&pb)[NRT]) __attribute__((always_inline)) {
+    // The keys' weights in fp16.
+    auto probs = [&](const f32x4 (&y)[NRT][2], float ks, float ve, float vr, u32x4 (&pb)[NRT]) __attribute__((always_inline)) {
         const float scale = a.scale_log2 * fmaxf(ks, kTinyScale);   // (above 0: a masked logit stays -inf)
-        const float ve = v_exponent(vs);
 #pragma unroll
         for (int rt = 0; rt < NRT; ++rt) {
-            float mx = y[rt][0][0];
+            f32x4 p[2], w[2];
+            key_weights(
+                y[rt], scale, ve, vr, M[rt], D[rt], L[rt], p, w, [](float, bool) {},
+                [&](float alpha) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, y[rt][e >> 2][e & 3]);
-            mx = __builtin_fmaf(mx, scale, ve);
-            if (__any(mx > M[rt] + kAbove)) {   // the wave's first tile, or a key far above the reference
-                mx = fmaxf(mx, shfl_xor_f(mx, 16));
-                mx = fmaxf(mx, shfl_xor_f(mx, 32));
-                const bool grow = mx > M[rt] + kAbove;
-                const float Mn = ceilf(mx) - kBelow;
-                const float alpha = grow ? fast_exp2(M[rt] - Mn) : 1.f;
-                M[rt] = grow ? Mn : M[rt];
-                L[rt] *= alpha;
-#pragma unroll
-                for (int jd = 0; jd < 8; ++jd) oacc[jd][rt] *= alpha;
-            }
-            float w[8], sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = fast_exp2(__builtin_fmaf(y[rt][e >> 2][e & 3], scale, -M[rt]));
-                sum += w[e];
-                w[e] *= vs;
-            }
-            L[rt] += sum;
-            pb[rt] = u32x4{pack_f16(w[0], w[1]), pack_f16(w[2], w[3]), pack_f16(w[4], w[5]), pack_f16(w[6], w[7])};
+                    for (int jd = 0; jd < 8; ++jd) oacc[jd][rt] *= alpha;
+                });
+            pb[rt] = u32x4{pack_f16(w[0][0], w[0][1]), pack_f16(w[0][2], w[0][3]), pack_f16(w[1][0], w[1][1]),
+                           pack_f16(w[1][2], w[1][3])};
         }
     };
     auto values = [&](const u32x2 (&v)[8], const u32x4 (&pb)[NRT]) __attribute__((always_inline)) {
@@ -183,10 +167,11 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
     auto load_v = [&](u32x2 (&v)[8], int t) __attribute__((always_inline)) {
         load_v_codes<true>(ca.c.v + tile_off(run, t), it.T - (it.key_begin + t * kTile), m16, G, v);
     };
-    auto scales = [&](int t, float& ks, float& vs) __attribute__((always_inline)) {
+    auto scales = [&](int t, float& ks, float& ve, float& vr) __attribute__((always_inline)) {
         const int l = (t - wave) / kWaves;
         ks = lane_f(run.ks, l);
-        vs = lane_f(run.vs, l);
+        ve = lane_f(run.ve, l);
+        vr = lane_f(run.vr, l);
     };
     if constexpr (NRT <= 2) {
         tile_pipeline<(NRT == 1 ? 3 : 2), KVCodes>(
@@ -198,10 +183,10 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
             [&](const KVCodes& b, int t) __attribute__((always_inline)) {
                 f32x4 y[NRT][2];
                 u32x4 pb[NRT];
-                float ks, vs;
-                scales(t, ks, vs);
+                float ks, ve, vr;
+                scales(t, ks, ve, vr);
                 logits(b.k, it.key_begin + t * kTile, y);
-                probs(y, ks, vs, pb);
+                probs(y, ks, ve, vr, pb);
                 values(b.v, pb);
             },
             start);
@@ -220,11 +205,11 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
         auto step = [&](int t, bool last) __attribute__((always_inline)) {
             f32x4 y[NRT][2];
             u32x4 pb[NRT];
-            float ks, vs;
-            scales(t, ks, vs);
+            float ks, ve, vr;
+            scales(t, ks, ve, vr);
             logits(k, it.key_begin + t * kTile, y);
             if (!last) load_k(k, t + kWaves);
-            probs(y, ks, vs, pb);
+            probs(y, ks, ve, vr, pb);
             values(v, pb);
             if (!last) load_v(v, t + kWaves);
         };
@@ -235,8 +220,8 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
         if (t < ntile) step(t, true);
     }
 
-    // The waves' statistics, then their partial outputs relative to the
-    // workgroup's row maxima: waves 0 and 1 put theirs into LDS, 2 and 3 add
+    // The waves' statistics, then their shares of the workgroup's partial
+    // output (see kPartialExp): waves 0 and 1 put theirs into LDS, 2 and 3 add
     // theirs, and the two sums are added on the way out.
 #pragma unroll
     for (int rt = 0; rt < NRT; ++rt) {
@@ -263,12 +248,12 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
                 float Mx = kEmpty;
 #pragma unroll
                 for (int u = 0; u < kWaves; ++u) Mx = fmaxf(Mx, lds.wml[u][row].x);
-                const float f = fast_exp2(M[rt] - Mx);
+                const int shift = partial_shift(M[rt], D[rt], Mx);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f32x4* at = &lds.o[wave & 1][row][8 * G + 2 * i];
-                    f32x4 w0 = f32x4{oacc[0][rt][i], oacc[1][rt][i], oacc[2][rt][i], oacc[3][rt][i]} * f;
-                    f32x4 w1 = f32x4{oacc[4][rt][i], oacc[5][rt][i], oacc[6][rt][i], oacc[7][rt][i]} * f;
+                    f32x4 w0 = times_2(f32x4{oacc[0][rt][i], oacc[1][rt][i], oacc[2][rt][i], oacc[3][rt][i]}, shift);
+                    f32x4 w1 = times_2(f32x4{oacc[4][rt][i], oacc[5][rt][i], oacc[6][rt][i], oacc[7][rt][i]}, shift);
                     if (turn) {
                         w0 += at[0];
                         w1 += at[1];
@@ -281,7 +266,8 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
         __syncthreads();
     }
     f32x4* po = reinterpret_cast<f32x4*>(a.part_o + (size_t)blockIdx.x * kRowCap * kHeadDim);
-    for (int x = threadIdx.x; x < R * (kHeadDim / 4); x += kThreads) po[x] = lds.o[0][x >> 5][x & 31] + lds.o[1][x >> 5][x & 31];
+    for (int x = threadIdx.x; x < R * (kHeadDim / 4); x += kThreads)
+        po[x] = lds.o[0][x >> 5][x & 31] + lds.o[1][x >> 5][x & 31];
 }
 
 // kMost: row tiles of the call's largest item.  Up to three (a SIMD holds two
@@ -351,7 +337,7 @@ __device__ __forceinline__ void finish_row(const VerifyArgs& a, int gr, f32x4 (*
     if (sg != 0) return;
 #pragma unroll
     for (int gq = 1; gq < kRowGroups; ++gq) mlo_merge(M, L, acc, gml[gq].x, gml[gq].y, red[gq][d4]);
-    const f32x4 o = acc * (1.f / L);
+    const f32x4 o = acc * (1.f / L) * kWhole;
     const int jl = row / a.group;
     const int h = c * a.group + (row - jl * a.group);
     const size_t base = (((size_t)b * a.max_q + a.qoff[bt] + jl) * a.n_q_heads + h) * kHeadDim + 4 * d4;

@@ -207,48 +207,6 @@ __device__ __forceinline__ void tile_probs(int rt, const f32x4 (&acc)[2], float 
     L[rt] += sum;
 }
 
-// The same over a coded cache, the reference as cc::v_exponent says; w: the
-// probabilities times V's scale.
-template <int NRT>
-__device__ __forceinline__ void tile_probs_coded(int rt, const f32x4 (&acc)[2], float scale, float vs, float* srow,
-                                                 int t, int wave, bool own_row, float (&M)[NRT], float (&L)[NRT],
-                                                 f32x4 (&oacc)[8][NRT], f32x4 (&p)[2], f32x4 (&w)[2]) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mx = fmaxf(mx, acc[e >> 2][e & 3]);
-    mx = __builtin_fmaf(mx, scale, cc::v_exponent(vs));
-    if (__any(mx > M[rt] + cc::kAbove)) {
-        mx = fmaxf(mx, shfl_xor_f(mx, 16));
-        mx = fmaxf(mx, shfl_xor_f(mx, 32));
-        const bool grow = mx > M[rt] + cc::kAbove;
-        const bool had = grow && M[rt] != kEmpty;
-        const float Mn = ceilf(mx) - cc::kBelow;
-        if (__any(had)) {
-            const float alpha = grow ? fast_exp2(M[rt] - Mn) : 1.f;
-            L[rt] *= alpha;
-#pragma unroll
-            for (int jd = 0; jd < 8; ++jd) oacc[jd][rt] *= alpha;
-            if (had && own_row) {   // this lane's stashed probabilities of the row
-                for (int tt = wave; tt < t; tt += kWaves) {
-                    f32x4* q = reinterpret_cast<f32x4*>(srow + tt * kTile);
-                    q[0] *= alpha;
-                    q[4] *= alpha;
-                }
-            }
-        }
-        M[rt] = grow ? Mn : M[rt];
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        p[e >> 2][e & 3] = fast_exp2(__builtin_fmaf(acc[e >> 2][e & 3], scale, -M[rt]));
-        sum += p[e >> 2][e & 3];
-    }
-    L[rt] += sum;
-    w[0] = p[0] * vs;
-    w[1] = p[1] * vs;
-}
-
 // The same for 16-bit codes: the reference follows the row's maximum over the
 // wave's tiles within 2^8 (kLazy), since a code spans 2^-54 .. 2^9 of it.
 constexpr float kLazy = 8.f;
@@ -376,12 +334,13 @@ __device__ __forceinline__ void stream_chunk(const StreamArgs& fa, const SChunk&
     if (tid == 0) *wait_failed = 0;
 
     float M[NRT], L[NRT];
+    float D[NRT];   // (coded: the reference of the weights, less M)
     f32x4 oacc[8][NRT];
     f32x4 plast[NRT][2];   // probabilities of the wave's last tile
 #pragma unroll
     for (int rt = 0; rt < NRT; ++rt) {
         M[rt] = kEmpty;
-        L[rt] = 0.f;
+        D[rt] = L[rt] = 0.f;
 #pragma unroll
         for (int jd = 0; jd < 8; ++jd) oacc[jd][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (!kU16) plast[rt][0] = plast[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -393,10 +352,11 @@ __device__ __forceinline__ void stream_chunk(const StreamArgs& fa, const SChunk&
         const int key0 = k.key_begin + t * kTile;
         u32x4 pb[NRT];
         float scale = a.scale_log2;
-        float vs = 1.f;
+        float v_exp = 0.f, v_rest = 1.f;   // V's scale
         if constexpr (kCode) {   // (above 0: a masked logit stays -inf)
             scale *= fmaxf(cc::lane_f(run.ks, (t - wave) / kWaves), cc::kTinyScale);
-            vs = cc::lane_f(run.vs, (t - wave) / kWaves);
+            v_exp = cc::lane_f(run.ve, (t - wave) / kWaves);
+            v_rest = cc::lane_f(run.vr, (t - wave) / kWaves);
             cc::decode_k<kCode == 2>(codes.k[0], kr[0]);
             cc::decode_k<kCode == 2>(codes.k[1], kr[1]);
         }
@@ -437,8 +397,23 @@ __device__ __forceinline__ void stream_chunk(const StreamArgs& fa, const SChunk&
                 }
             } else {
                 f32x4 w[2];
-                if constexpr (kCode) tile_probs_coded<NRT>(rt, acc, scale, vs, srow, t, wave, own, M, L, oacc, p, w);
-                else tile_probs<NRT>(rt, acc, scale, srow, t, wave, own, M, L, oacc, p);
+                if constexpr (kCode)
+                    cc::key_weights(
+                        acc, scale, v_exp, v_rest, M[rt], D[rt], L[rt], p, w,
+                        [&](float alpha, bool had) __attribute__((always_inline)) {
+                            if (!had || !own) return;
+                            for (int tt = wave; tt < t; tt += kWaves) {   // this lane's stashed probabilities of the row
+                                f32x4* q = reinterpret_cast<f32x4*>(srow + tt * kTile);
+                                q[0] *= alpha;
+                                q[4] *= alpha;
+                            }
+                        },
+                        [&](float alpha) __attribute__((always_inline)) {
+#pragma unroll
+                            for (int jd = 0; jd < 8; ++jd) oacc[jd][rt] *= alpha;
+                        });
+                else
+                    tile_probs<NRT>(rt, acc, scale, srow, t, wave, own, M, L, oacc, p);
                 if constexpr (kCode)
                     pb[rt] = u32x4{cc::pack_f16(w[0][0], w[0][1]), cc::pack_f16(w[0][2], w[0][3]), cc::pack_f16(w[1][0], w[1][1]),
                                    cc::pack_f16(w[1][2], w[1][3])};
@@ -559,14 +534,17 @@ __device__ __forceinline__ void stream_chunk(const StreamArgs& fa, const SChunk&
         float mw = kEmpty;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) mw = fmaxf(mw, wml[w * kRowCap + rt * 16 + m16].x);
-        const float f = fast_exp2(M[rt] - mw);
+        const float f = kCode ? 0.f : fast_exp2(M[rt] - mw);
+        const int shift = kCode ? cc::partial_shift(M[rt], D[rt], mw) : 0;
         const int pr = tid >> 4, c2 = tid & 15;
         uint64_t* po = reinterpret_cast<uint64_t*>(a.part_o + (k.row0 + (size_t)k.s * R + rt * 16 + pr) * kHeadDim);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             f32x4* dst = reinterpret_cast<f32x4*>(park + (wave * 16 + m16) * kParkStride + 8 * G);
-            dst[0] = f32x4{oacc[0][rt][i], oacc[1][rt][i], oacc[2][rt][i], oacc[3][rt][i]} * f;
-            dst[1] = f32x4{oacc[4][rt][i], oacc[5][rt][i], oacc[6][rt][i], oacc[7][rt][i]} * f;
+            const f32x4 o0 = {oacc[0][rt][i], oacc[1][rt][i], oacc[2][rt][i], oacc[3][rt][i]};
+            const f32x4 o1 = {oacc[4][rt][i], oacc[5][rt][i], oacc[6][rt][i], oacc[7][rt][i]};
+            dst[0] = kCode ? cc::times_2(o0, shift) : o0 * f;
+            dst[1] = kCode ? cc::times_2(o1, shift) : o1 * f;
             __syncthreads();
             float2 o = *reinterpret_cast<const float2*>(park + pr * kParkStride + 2 * c2);
 #pragma unroll
@@ -780,7 +758,8 @@ __device__ __forceinline__ void stream_chunk(const StreamArgs& fa, const SChunk&
         // eight groups of 32 lanes: gp of them per row, chunks sub, sub + gp, ...
         const int nrp = nr > 4 ? 8 : nr > 2 ? 4 : nr;
         const int gp = 8 / nrp, sg = tid >> 5, d4 = tid & 31, sub = sg % gp;
-        auto write_row = [&](int r2, const f32x4& o) {
+        auto write_row = [&](int r2, f32x4 o) {
+            if constexpr (kCode) o *= cc::kWhole;
             const int jl = r2 / g, h = k.c * g + (r2 - jl * g);
             const int dim = 32 * ((d4 >> 1) & 3) + 8 * (d4 >> 3) + 4 * (d4 & 1);
             const size_t base = (((size_t)k.b * a.max_q + k.qoff + jl) * a.n_q_heads + h) * kHeadDim + dim;

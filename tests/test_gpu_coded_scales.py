@@ -1,0 +1,115 @@
+"""Coded attention over caches whose scales lie anywhere that the append, or a
+caller, may put them: what one call writes the others read.
+
+Bars are those of test_gpu_coded: verify's weights are fp16 relative to their
+row's largest, |dO| <= 2^-9 sum P|v| + the weights' absolute step
+(coded_reference.weight_floor), scores within 1e-3 of each score."""
+import numpy as np
+import pytest
+import torch
+
+import coded_reference as ref
+from gpu_common import check_scores
+from paper_2607_27735_amd import binding as B
+from test_gpu_coded import CODES, MODES, SM, code_cache, host, ints, on_gpu
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU visible", allow_module_level=True)
+
+
+def check_verify(c: ref.Cache, q, q_len, mode, cus=0, sm=SM, out_fp32=True):
+    """verify over c against the plain form; c is what the GPU's cache holds."""
+    cache, table = on_gpu(c)
+    p = B.make_params(sm, out_fp32=out_fp32, verify_mode=mode)
+    try:
+        B.set_cu_budget(cus)
+        out, sc = B.verify_attn_coded(q.cuda(), cache, table, c.max_ctx, c.ctx, q_len, p)
+    finally:
+        B.set_cu_budget(0)
+    torch.cuda.synchronize()
+    o, s, q64 = out.double().cpu().numpy(), sc.double().cpu().numpy(), q.double().numpy()
+    want, oabs, sh = ref.verify(c, q64, q_len, sm, 16)
+    batch, hq = q.shape[0], q.shape[2]
+    live = np.arange(q.shape[1])[None, :, None] < np.array(q_len)[:, None, None] * np.ones((1, 1, hq), bool)
+    assert np.all(np.isfinite(o[live])), f"{int((~np.isfinite(o[live])).sum())} outputs are not finite"
+    bound = 2.0 ** -9 * oabs + ref.weight_floor(c, q64, q_len, sm) + (0 if out_fp32 else 2.0 ** -8) * np.abs(want)
+    over = (np.abs(o - want) / bound)[live].max()
+    assert over <= 1, f"{over:.2f} times the bar"
+    check_scores(s, sh.reshape(batch, c.n_kv, hq // c.n_kv, -1).sum(2), c.ctx)
+    return o, want
+
+
+def appended(rng, code, ctx, edit, n_kv=2, page=64, block=32):
+    """A cache filled by the append from rows that edit(k, v) has changed, read back."""
+    c = ref.Cache(rng, ctx, n_kv, page, block, code)
+    cache = code_cache(np.zeros_like(c.k), np.zeros_like(c.v), np.zeros_like(c.ks), np.zeros_like(c.vs), code)
+    slots = np.concatenate([c.table[b, np.arange(t) // page] * page + np.arange(t) % page for b, t in enumerate(ctx)])
+    k, v = (rng.standard_normal((sum(ctx), n_kv, 128)).astype(np.float32) for _ in range(2))
+    edit(k, v)
+    up = lambda x: torch.from_numpy(x).to(torch.bfloat16).cuda()
+    B.cache_append(cache, up(k), up(v), ints(slots))
+    torch.cuda.synchronize()
+    c.k, c.v, c.ks, c.vs = host(cache)
+    return c
+
+
+def huge(k, v):
+    v[5, 0, 7], v[200, 1, 9], v[303, 0, 100] = np.inf, -np.inf, np.inf   # (bf16's largest)
+    v[77, :, 3] = 2.0 ** 119
+    v[130, 0] = 2.0 ** 118
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("code", CODES)
+def test_verify_reads_what_the_append_writes(code, mode):
+    """Infinities and values near fp32's largest in V: they count by their share of
+    their own column, and every other element is as if they were not there."""
+    c = appended(np.random.default_rng(1), code, [400, 70], huge)
+    assert c.vs.max() == 2.0 ** (120 if code == "e4m3" else 122)
+    # (flat rows: no key has more than a hundredth, so that no column passes fp32's range)
+    q, _ = ref.bf16_normal(np.random.default_rng(2), 2, 5, 8, 128, scale=0.5)
+    check_verify(c, q, [5, 2], MODES[mode])
+    check_verify(c, q, [5, 2], MODES[mode], cus=1)
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("low,high", [(-70, 90), (-126, 100), (60, 116), (-126, -100)])
+def test_verify_scales_of_any_size(low, high, code, mode):
+    """V's scales from block to block anywhere between 2^low and 2^high: a key's
+    share of its row's sum and scores does not depend on V."""
+    rng = np.random.default_rng(high + 200)
+    c = ref.Cache(rng, [700, 333], 2, 64, 32, code)
+    c.vs[...] = np.where(np.isnan(c.vs), c.vs, 2.0 ** rng.integers(low, high + 1, c.vs.shape))
+    q, _ = ref.bf16_normal(rng, 2, 6, 8, 128, scale=1.5)
+    check_verify(c, q, [6, 3], MODES[mode])
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("low,high", [(-20, 120), (-80, 100), (-126, 110)])
+def test_verify_far_scales_against_steep_logits(low, high, code, mode):
+    """Keys that grow less likely by 2^-5 each while their block's V grows: their
+    weights are alike though their probabilities are 2^150 apart.  (Scores below
+    fp32's least normal number are not looked at.)"""
+    c = ref.Cache(np.random.default_rng(3), [96], 1, 32, 32, code)
+    one = 0x38 if code == "e4m3" else 0x01
+    for j in range(3):      # three blocks; the keys of one have one logit
+        pg = c.table[0, j]
+        c.k[pg, 0], c.ks[pg, 0] = 0, 1.0
+        c.k[pg, 0, :, 0] = one
+        c.ks[pg, 0, 0] = [3.0, 2.0, 1.0][j]
+        c.vs[pg, 0, 0] = 2.0 ** [low, (low + high) // 2, high][j]
+    q = torch.zeros(1, 1, 4, 128, dtype=torch.bfloat16)
+    step = (high - low) / 2 * np.log(2) / SM            # (a block's step in log2 units: (high - low) / 2)
+    q[..., 0] = torch.tensor([step, step * 0.98, step * 1.02, 1.0])
+    cache, table = on_gpu(c)
+    out, _ = B.verify_attn_coded(q.cuda(), cache, table, 96, [96], [1], B.make_params(SM, out_fp32=True, verify_mode=MODES[mode]))
+    torch.cuda.synchronize()
+    q64 = q.double().numpy()
+    want, oabs, _ = ref.verify(c, q64, [1], SM, 16)
+    bound = 2.0 ** -9 * oabs + ref.weight_floor(c, q64, [1], SM)
+    over = np.abs(out.double().cpu().numpy() - want) / bound
+    assert over.max() <= 1, f"{over.max():.2f} times the bar"
