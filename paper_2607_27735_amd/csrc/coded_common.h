@@ -18,7 +18,13 @@ namespace cc {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kRowBytes = kHeadDim;   // a cached row
-constexpr float kTinyScale = 1e-37f;  // least scale of K, so that a masked logit times it stays -inf
+
+// A logit's factor, sm_scale log2(e) times K's scale: above 0, whatever the two, so
+// that a masked logit times it stays -inf (0 times it would be NaN).
+__device__ __forceinline__ float logit_scale(float scale_log2, float ks) {
+    constexpr float kLeast = 0x1p-126f;
+    return fmaxf(scale_log2 * ks, kLeast);
+}
 
 // Four codes of a dword as two packed bf16 pairs.
 template <bool kInt8>

@@ -129,7 +129,7 @@ __device__ __forceinline__ void sweep_item(const CodedVerifyArgs& ca, const Item
     };
     // The keys' weights in fp16.
     auto probs = [&](const f32x4 (&y)[NRT][2], float ks, float ve, float vr, u32x4 (&pb)[NRT]) __attribute__((always_inline)) {
-        const float scale = a.scale_log2 * fmaxf(ks, kTinyScale);   // (above 0: a masked logit stays -inf)
+        const float scale = logit_scale(a.scale_log2, ks);
 #pragma unroll
         for (int rt = 0; rt < NRT; ++rt) {
             f32x4 p[2], w[2];
@@ -420,7 +420,7 @@ __device__ __forceinline__ void score_item(const CodedVerifyArgs& ca, const Item
         for (int rt = 0; rt < NRT; ++rt) lse[rt] = *reinterpret_cast<const f32x4*>(&lse_row[rt * 16 + 4 * G]);
     };
     auto tile_scores = [&](const KCodes& b, int key0, float ks) __attribute__((always_inline)) {
-        const float scale = a.scale_log2 * fmaxf(ks, kTinyScale);
+        const float scale = logit_scale(a.scale_log2, ks);
         const int place = q_place(m16, G);
         f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
         // Both half tiles for each read of the rows; with three row tiles, which

@@ -353,8 +353,8 @@ __device__ __forceinline__ void stream_chunk(const StreamArgs& fa, const SChunk&
         u32x4 pb[NRT];
         float scale = a.scale_log2;
         float v_exp = 0.f, v_rest = 1.f;   // V's scale
-        if constexpr (kCode) {   // (above 0: a masked logit stays -inf)
-            scale *= fmaxf(cc::lane_f(run.ks, (t - wave) / kWaves), cc::kTinyScale);
+        if constexpr (kCode) {
+            scale = cc::logit_scale(scale, cc::lane_f(run.ks, (t - wave) / kWaves));
             v_exp = cc::lane_f(run.ve, (t - wave) / kWaves);
             v_rest = cc::lane_f(run.vr, (t - wave) / kWaves);
             cc::decode_k<kCode == 2>(codes.k[0], kr[0]);

@@ -113,3 +113,18 @@ def test_verify_far_scales_against_steep_logits(low, high, code, mode):
     bound = 2.0 ** -9 * oabs + ref.weight_floor(c, q64, [1], SM)
     over = np.abs(out.double().cpu().numpy() - want) / bound
     assert over.max() <= 1, f"{over.max():.2f} times the bar"
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("sm", [SM, 1e-9, 1e-37])
+def test_verify_masks_keys_whose_logits_scale_to_nothing(sm, code, mode):
+    """The last block, which some rows do not see all of, is of zero keys (the append
+    gives them the scale 2^-126, a caller may give 0): masked is masked, however
+    small the logits' factor."""
+    rng = np.random.default_rng(6)
+    c = ref.Cache(rng, [300, 31], 2, 64, 32, code)
+    c.ks[c.table[0, 4], 0], c.ks[c.table[0, 4], 1] = 2.0 ** -126, 0.0
+    c.ks[c.table[1, 0], 0, 0], c.ks[c.table[1, 0], 1, 0] = 0.0, 2.0 ** -126
+    q, _ = ref.bf16_normal(rng, 2, 6, 8, 128, scale=1.5)
+    check_verify(c, q, [6, 6], MODES[mode], sm=sm)
