@@ -643,7 +643,7 @@ int ssl_verify_attn_coded(const ssl_shape *shape, const ssl_params *params,
  * Draft attention, and a step of a draft round, over a coded cache: as
  * ssl_draft_attn_paged and ssl_draft_step_paged (fixed rows through idx), with
  * keys and values code * scale; the value product uses the probabilities times
- * V's scale, to 16 bits (two bf16 numbers).  Workspaces from ssl_draft_workspace and
+ * V's scale, to 16 bits (two bf16 numbers).  V's scales as for verify.  Workspaces from ssl_draft_workspace and
  * ssl_draft_step_workspace.  Other errors as there, and those of the
  * cache's sizes as in ssl_cache_append.
  */

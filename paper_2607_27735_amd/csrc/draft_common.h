@@ -160,6 +160,10 @@ __device__ __forceinline__ void coded_logits(float scale_log2, const u32x4 (&qop
 // as coarse as a bf16 output and far coarser than an fp32 one, and bf16 has fp32's
 // range, so that scales may lie anywhere.  (us per call, one number / two: 16384
 // entries 7.7 / 7.9; 262144 of int8 18.8 / 18.4; 512512 31.1 / 29.7.)
+// The reference is 12 above the row's largest logit, so that values near fp32's
+// largest (the append's for an infinity is 2^128) do not pass its range before the
+// row is divided by its sum.
+constexpr float kHeadroom = 12.f;
 template <bool kInt8>
 __device__ __forceinline__ void coded_values(const float (&y)[8], const cc::u32x2 (&v)[8], float my_vs, int p0, int G, float& M,
                                              float& L, f32x4 (&oacc)[8]) {
@@ -168,7 +172,7 @@ __device__ __forceinline__ void coded_values(const float (&y)[8], const cc::u32x
     for (int e = 1; e < 8; ++e) mt = fmaxf(mt, y[e]);
     mt = fmaxf(mt, shfl_xor_f(mt, 16));
     mt = fmaxf(mt, shfl_xor_f(mt, 32));
-    const float Mn = fmaxf(M, mt);
+    const float Mn = fmaxf(M, mt + kHeadroom);
     const float alpha = fast_exp2(M - Mn);   // M = -inf on the first tile: alpha = 0
     float p[8], sum = 0.f;
 #pragma unroll

@@ -12,6 +12,7 @@ import torch
 import coded_reference as ref
 from paper_2607_27735_amd import binding as B
 from test_gpu_coded import CODES, SM, index_sets, ints, on_gpu
+from test_gpu_coded_scales import appended
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +52,25 @@ def test_flat_rows(budget, code, pow2):
             assert over <= 1, f"{over:.2f} times the bar"
     o, want, oabs = run(c, idx, n, q, 2, budget, out_fp32=False)
     assert np.all(np.abs(o - want) <= 2.0 ** -12 * oabs + 2.0 ** -8 * np.abs(want) * (1 + 2.0 ** -8))
+
+
+def huge(k, v):
+    v[5, 0, 7], v[200, 1, 9], v[303, 0, 100] = np.inf, -np.inf, np.inf   # (bf16's largest)
+    v[77, :, 3] = 2.0 ** 119
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_reads_what_the_append_writes(code):
+    """Infinities and values near fp32's largest in V, in keys that are their row's
+    likeliest and in others: finite where the plain form is."""
+    c = appended(np.random.default_rng(1), code, [400, 70], huge)
+    rng = np.random.default_rng(2)
+    idx, n = index_sets(rng, c.ctx, 2, 400)
+    q, q64 = ref.bf16_normal(rng, 2, 8, 128, scale=0.25)
+    for head, key in ((0, 5), (1, 303), (5, 200), (6, 77)):   # rows that give one of them the most, about a third
+        k = c.values("k", 0, head // 4, np.array([key]))[0]
+        q[0, head] = torch.from_numpy(k * (5.3 / SM / (k @ k))).to(torch.bfloat16)
+    o, want, oabs = run(c, idx, n, q, 2, 400)
+    fits = np.abs(want) < 2.0 ** 127.9
+    assert fits.all() and np.all(np.isfinite(o)), f"{int((~np.isfinite(o)).sum())} outputs are not finite"
+    assert np.all(np.abs(o - want) <= 2.0 ** -9 * oabs)
