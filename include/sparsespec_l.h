@@ -548,10 +548,13 @@ typedef struct {
  *   - total_len[b] = ctx + new where served, else ctx: a caller sees there who
  *     was not;
  *   - free_range_out = {free_range[0] + pages taken, free_range[1]}.
+ * ssl_page_map_bounded is the same call with the length of the free list
+ * (n_free_pages >= 0, SSL_ERR_SHAPE otherwise): pages that free_range claims past
+ * it count as none, so no range on the device makes the call read behind the list.
  * All arrays are int32 in device memory: ctx_len, new_len, total_len [batch],
  * block_table [batch][max_blocks], slot_map [max_tokens], row_start
  * [batch + 1], free_range and free_range_out [2] (0 <= first <= end, end at most
- * the list's length).  Page ids are not checked.  The outputs must not overlap
+ * the list's length, which ssl_page_map is not told).  Page ids are not checked.  The outputs must not overlap
  * the inputs (SSL_ERR_SHAPE where total_len is ctx_len or new_len, or
  * free_range_out is free_range).  No workspace.  Errors: SSL_ERR_NULL;
  * SSL_ERR_SHAPE if batch, page_size or max_blocks < 1, max_tokens < 0 or
@@ -563,6 +566,11 @@ int ssl_page_map(int32_t batch, int32_t page_size, int32_t max_blocks, int32_t m
                  const int32_t *free_pages, const int32_t *free_range, int32_t *slot_map,
                  int32_t *row_start, int32_t *total_len, int32_t *free_range_out,
                  hipStream_t stream);
+int ssl_page_map_bounded(int32_t batch, int32_t page_size, int32_t max_blocks, int32_t max_tokens,
+                         int32_t n_free_pages, const int32_t *ctx_len, const int32_t *new_len,
+                         int32_t *block_table, const int32_t *free_pages,
+                         const int32_t *free_range, int32_t *slot_map, int32_t *row_start,
+                         int32_t *total_len, int32_t *free_range_out, hipStream_t stream);
 
 /*
  * Codes the K and V rows of n_tokens new tokens into their slots.

@@ -44,7 +44,7 @@ EXPORTED = [
     "ssl_verify_attn_paged", "ssl_draft_attn_paged",
     "ssl_draft_materialize", "ssl_draft_step_workspace", "ssl_draft_step",
     "ssl_draft_materialize_paged", "ssl_draft_step_paged",
-    "ssl_page_map", "ssl_cache_append", "ssl_verify_coded_workspace", "ssl_verify_coded_plan",
+    "ssl_page_map", "ssl_page_map_bounded", "ssl_cache_append", "ssl_verify_coded_workspace", "ssl_verify_coded_plan",
     "ssl_verify_attn_coded", "ssl_draft_attn_coded", "ssl_draft_step_coded",
     "ssl_logit_stats_workspace", "ssl_logit_stats", "ssl_greedy_accept_workspace",
     "ssl_greedy_accept", "ssl_spec_accept_workspace", "ssl_spec_accept",
@@ -153,6 +153,7 @@ def load(path: Optional[str] = None):
                                          _vp, _vp, _vp, _vp, _vp, _sz, _vp]
     kp = ctypes.POINTER(CodedCacheArgs)
     lib.ssl_page_map.argtypes = [_i32] * 4 + [_vp] * 10
+    lib.ssl_page_map_bounded.argtypes = [_i32] * 5 + [_vp] * 10
     lib.ssl_cache_append.argtypes = [kp, _i32, _i32, _vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp, _vp]
     lib.ssl_verify_coded_workspace.argtypes = [sp, pp, _i32p, _i32p, _szp]
     lib.ssl_verify_coded_plan.argtypes = [sp, pp, _i32p, _i32p, _i32p, _i32p, _i32p]
@@ -173,7 +174,7 @@ def load(path: Optional[str] = None):
               "ssl_select_draft", "ssl_draft_workspace", "ssl_draft_attn", "ssl_draft_materialize",
               "ssl_draft_step_workspace", "ssl_draft_step", "ssl_verify_attn_paged",
               "ssl_draft_attn_paged", "ssl_draft_materialize_paged", "ssl_draft_step_paged",
-              "ssl_page_map", "ssl_cache_append", "ssl_verify_coded_workspace",
+              "ssl_page_map", "ssl_page_map_bounded", "ssl_cache_append", "ssl_verify_coded_workspace",
               "ssl_verify_coded_plan", "ssl_verify_attn_coded", "ssl_draft_attn_coded", "ssl_draft_step_coded",
               "ssl_logit_stats_workspace",
               "ssl_logit_stats", "ssl_greedy_accept_workspace", "ssl_greedy_accept",
@@ -1177,7 +1178,7 @@ def _workspace_of(workspace: Optional[torch.Tensor], need: int, device, stream) 
 
 
 class PreparedPageMap:
-    """ssl_page_map over fixed device buffers: pages and slots for one step's
+    """ssl_page_map_bounded over fixed device buffers: pages and slots for one step's
     tokens from the lengths in ``ctx_len`` and ``new_len``.  All tensors int32:
     ctx_len, new_len, total_len [B], block_table [B, max_blocks], free_pages
     [any], free_range and free_range_out [2], slot_map [max_tokens], row_start
@@ -1186,7 +1187,7 @@ class PreparedPageMap:
 
     def __init__(self, ctx_len, new_len, block_table, free_pages, free_range, page_size: int, slot_map,
                  row_start, total_len, free_range_out, stream=None):
-        self._call = load().ssl_page_map
+        self._call = load().ssl_page_map_bounded
         ts = (ctx_len, new_len, block_table, free_pages, free_range, slot_map, row_start, total_len, free_range_out)
         _need_gpu(*ts)
         _one_device(*ts)
@@ -1200,11 +1201,11 @@ class PreparedPageMap:
             raise ValueError("free_range and free_range_out are (first, end)")
         self.tensors = ts
         self.device = ctx_len.device
-        self._a = (batch, int(page_size), width, slot_map.numel(), *(t.data_ptr() for t in ts), _stream(stream))
+        self._a = (batch, int(page_size), width, slot_map.numel(), free_pages.numel(), *(t.data_ptr() for t in ts), _stream(stream))
 
     def run(self) -> None:
         if rc := self._call(*self._a):
-            _check(rc, "ssl_page_map")
+            _check(rc, "ssl_page_map_bounded")
 
 
 def page_map(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,

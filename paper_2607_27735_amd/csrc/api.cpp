@@ -1757,10 +1757,20 @@ int ssl_draft_step_paged(const ssl_shape* shape, const ssl_params* params,
 int ssl_page_map(int32_t batch, int32_t page_size, int32_t max_blocks, int32_t max_tokens, const int32_t* ctx_len,
                  const int32_t* new_len, int32_t* block_table, const int32_t* free_pages, const int32_t* free_range,
                  int32_t* slot_map, int32_t* row_start, int32_t* total_len, int32_t* free_range_out, hipStream_t stream) {
-    if (batch < 1 || page_size < 1 || max_blocks < 1 || max_tokens < 0) return SSL_ERR_SHAPE;
+    return ssl_page_map_bounded(batch, page_size, max_blocks, max_tokens, INT32_MAX, ctx_len, new_len, block_table, free_pages,
+                                free_range, slot_map, row_start, total_len, free_range_out, stream);
+}
+
+int ssl_page_map_bounded(int32_t batch, int32_t page_size, int32_t max_blocks, int32_t max_tokens, int32_t n_free_pages,
+                         const int32_t* ctx_len, const int32_t* new_len, int32_t* block_table, const int32_t* free_pages,
+                         const int32_t* free_range, int32_t* slot_map, int32_t* row_start, int32_t* total_len,
+                         int32_t* free_range_out, hipStream_t stream) {
+    if (batch < 1 || page_size < 1 || max_blocks < 1 || max_tokens < 0 || n_free_pages < 0) return SSL_ERR_SHAPE;
     if ((int64_t)page_size * max_blocks > INT32_MAX) return SSL_ERR_SHAPE;
     if (batch > kMapBatch || max_tokens >= (1 << 30)) return SSL_ERR_UNSUPPORTED;
-    const void* all[] = {ctx_len, new_len, block_table, free_pages, free_range, row_start, total_len, free_range_out};
+    if (n_free_pages > 0 && !free_pages) return SSL_ERR_NULL;
+    if (!aligned(free_pages, 4)) return SSL_ERR_ALIGN;
+    const void* all[] = {ctx_len, new_len, block_table, free_range, row_start, total_len, free_range_out};
     for (const void* p : all) {
         if (!p) return SSL_ERR_NULL;
         if (!aligned(p, 4)) return SSL_ERR_ALIGN;
@@ -1783,6 +1793,7 @@ int ssl_page_map(int32_t batch, int32_t page_size, int32_t max_blocks, int32_t m
     a.page_size = page_size;
     a.max_blocks = max_blocks;
     a.max_tokens = max_tokens;
+    a.n_free = n_free_pages;
     return hip_rc(launch_page_map(a, stream));
 }
 

@@ -69,8 +69,10 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
         c[i] = b < a.batch ? a.ctx_len[b] : 0;
         n[i] = b < a.batch ? a.new_len[b] : 0;
     }
+    // (the range is the device's word: pages that it claims past the list are not there)
     const int first = a.free_range[0], end = a.free_range[1];
-    const int avail = first >= 0 ? min(max(end - first, 0), kMapFar - 1) : 0;
+    const int last = min(end, a.n_free);
+    const int avail = first >= 0 && first < last ? min(last - first, kMapFar - 1) : 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int64_t total = (int64_t)c[i] + n[i];
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
                     const int blk = pos / a.page_size, fresh = blk - held[b];
                     const int page = fresh >= 0 ? a.free_pages[first + (b ? pages[b - 1] : 0) + fresh]
                                                 : a.block_table[(size_t)b * a.max_blocks + blk];
-                    slot = page * a.page_size + (pos - blk * a.page_size);
+                    slot = (int)((uint32_t)page * (uint32_t)a.page_size + (uint32_t)(pos - blk * a.page_size));   // (any page id)
                 }
             }
             a.slot_map[t] = slot;

@@ -202,6 +202,7 @@ struct PageMapArgs {
     int32_t* total_len;          // [batch]
     int32_t* free_range_out;
     int32_t batch, page_size, max_blocks, max_tokens;
+    int32_t n_free;              // entries of free_pages (INT32_MAX: not known)
 };
 
 // Rows to code into a coded cache (see cache_append_kernel); window is set by
