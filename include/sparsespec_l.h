@@ -555,8 +555,8 @@ typedef struct {
  * block_table [batch][max_blocks], slot_map [max_tokens], row_start
  * [batch + 1], free_range and free_range_out [2] (0 <= first <= end, end at most
  * the list's length, which ssl_page_map is not told).  Page ids are not checked.  The outputs must not overlap
- * the inputs (SSL_ERR_SHAPE where total_len is ctx_len or new_len, or
- * free_range_out is free_range).  No workspace.  Errors: SSL_ERR_NULL;
+ * the inputs or each other (SSL_ERR_SHAPE; ssl_page_map cannot tell for free_pages).
+ * No workspace.  Errors: SSL_ERR_NULL;
  * SSL_ERR_SHAPE if batch, page_size or max_blocks < 1, max_tokens < 0 or
  * page_size * max_blocks > 2^31 - 1; SSL_ERR_UNSUPPORTED if batch > 1024
  * or max_tokens >= 2^30; SSL_ERR_ALIGN.

@@ -1777,8 +1777,21 @@ int ssl_page_map_bounded(int32_t batch, int32_t page_size, int32_t max_blocks, i
     }
     if (max_tokens > 0 && !slot_map) return SSL_ERR_NULL;
     if (!aligned(slot_map, 4)) return SSL_ERR_ALIGN;
-    // (every workgroup reads the lengths and the range, one writes these)
-    if (total_len == ctx_len || total_len == new_len || free_range_out == free_range) return SSL_ERR_SHAPE;
+    // Every workgroup reads the inputs while others write: what is written may
+    // overlap nothing else.
+    struct Span {
+        const void* p;
+        int64_t n;   // int32 entries
+    };
+    const int64_t listed = n_free_pages == INT32_MAX ? 0 : n_free_pages;   // (ssl_page_map does not know)
+    const Span spans[] = {{block_table, (int64_t)batch * max_blocks}, {slot_map, max_tokens}, {row_start, batch + 1},
+                          {total_len, batch}, {free_range_out, 2},
+                          {ctx_len, batch}, {new_len, batch}, {free_range, 2}, {free_pages, listed}};
+    for (int i = 0; i < 5; ++i)
+        for (int j = i + 1; j < 9; ++j) {
+            const char *x = static_cast<const char*>(spans[i].p), *y = static_cast<const char*>(spans[j].p);
+            if (spans[i].n > 0 && spans[j].n > 0 && x < y + 4 * spans[j].n && y < x + 4 * spans[i].n) return SSL_ERR_SHAPE;
+        }
     PageMapArgs a = {};
     a.ctx_len = ctx_len;
     a.new_len = new_len;

@@ -28,6 +28,48 @@ def test_refusals_of_the_bounded_call():
     assert bounded(n_free=0, free=None, total=FAKE) == B.SSL_ERR_SHAPE   # total_len is ctx_len
 
 
+SIZES = dict(table=16, slots=32, rows=3, total=2, out=2, ctx=2, new=2, rng=2, free=16)   # int32 entries of bounded()'s call
+OUTPUTS = ("table", "slots", "rows", "total", "out")
+
+
+@pytest.mark.parametrize("written", OUTPUTS)
+@pytest.mark.parametrize("other", list(SIZES))
+def test_overlaps_are_refused(written, other):
+    """An output that shares its first or last entry with anything else."""
+    if other == written:
+        return
+    at = FAKE + 0x100000
+    for shift in (4 * (SIZES[other] - 1), -4 * (SIZES[written] - 1)):
+        assert bounded(**{other: at, written: at + shift}) == B.SSL_ERR_SHAPE
+        if other != "free":
+            p = dict(ctx=FAKE, new=FAKE + 4096, table=FAKE + 8192, free=FAKE + 12288, rng=FAKE + 16384, slots=FAKE + 20480,
+                     rows=FAKE + 24576, total=FAKE + 28672, out=FAKE + 32768)
+            p.update({other: at, written: at + shift})
+            assert B.load().ssl_page_map(2, 64, 8, 32, *p.values(), None) == B.SSL_ERR_SHAPE
+
+
+@pytest.mark.gpu
+def test_neighbours_in_one_buffer():
+    """All arrays side by side in one allocation: none overlaps."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    buf = torch.zeros(sum(SIZES.values()), dtype=torch.int32, device="cuda")
+    t, at = {}, 0
+    for name, n in SIZES.items():
+        t[name] = buf[at:at + n]
+        at += n
+    t["ctx"].copy_(torch.tensor([3, 70]))
+    t["new"].copy_(torch.tensor([2, 60]))
+    t["rng"].copy_(torch.tensor([0, 16]))
+    t["free"].copy_(torch.arange(100, 116))
+    t["table"].view(2, 8)[0, 0], t["table"].view(2, 8)[1, 0], t["table"].view(2, 8)[1, 1] = 5, 6, 7
+    B.PreparedPageMap(t["ctx"], t["new"], t["table"].view(2, 8), t["free"], t["rng"], 64, t["slots"], t["rows"], t["total"],
+                      t["out"]).run()
+    torch.cuda.synchronize()
+    assert t["total"].tolist() == [5, 70] and t["slots"].tolist() == [5 * 64 + 3, 5 * 64 + 4] + [-1] * 30
+    assert t["rows"].tolist() == [0, 2, 62] and t["out"].tolist() == [0, 16] and t["ctx"].tolist() == [3, 70]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch", [3, 300])
 @pytest.mark.parametrize("first,end", [(0, 5), (2, 40), (2, 2 ** 31 - 1), (7, 9), (12, 14), (0, -1), (2 ** 31 - 1, -2 ** 31),
