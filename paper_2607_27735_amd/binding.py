@@ -1125,6 +1125,8 @@ class CodeCache:
     def empty(cls, n_pages: int, n_kv_heads: int, page_size: int, scale_block: int,
               dtype: torch.dtype = torch.float8_e4m3fn, device="cuda") -> "CodeCache":
         """A cache of zeros."""
+        if scale_block < 1 or page_size < scale_block or page_size % scale_block:
+            raise ValueError("page_size must be a multiple of scale_block")
         shape = (n_pages, n_kv_heads, page_size, 128)
         k, v = (torch.zeros(shape, dtype=torch.int8, device=device).view(dtype) for _ in range(2))
         ks, vs = (torch.zeros(n_pages, n_kv_heads, page_size // scale_block, device=device) for _ in range(2))

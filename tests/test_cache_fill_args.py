@@ -1,4 +1,4 @@
-"""The page map against free ranges and buffers that a caller got wrong: what the
+"""The 8-bit cache's fillers against ranges, buffers and sizes that a caller got wrong: what the
 device's words claim never makes the call read behind the free list."""
 import ctypes
 
@@ -46,6 +46,13 @@ def test_overlaps_are_refused(written, other):
                      rows=FAKE + 24576, total=FAKE + 28672, out=FAKE + 32768)
             p.update({other: at, written: at + shift})
             assert B.load().ssl_page_map(2, 64, 8, 32, *p.values(), None) == B.SSL_ERR_SHAPE
+
+
+@pytest.mark.parametrize("page,block", [(128, 48), (64, 128), (64, 0), (64, -32), (100, 32)])
+def test_an_empty_cache_keeps_to_its_scale_block(page, block):
+    """A page of 128 tokens has no blocks of 48: not a cache whose blocks are of 64."""
+    with pytest.raises(ValueError):
+        B.CodeCache.empty(4, 2, page, block, device="cpu")
 
 
 @pytest.mark.gpu
