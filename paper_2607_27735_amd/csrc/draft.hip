@@ -105,11 +105,11 @@ __device__ __forceinline__ uint32_t coded_row(const DraftArgs& a, int b, int kvc
 // a CU holds two workgroups even at four tiles per wave (the 8B batch-8
 // workload's draft: 46.7 -> 25.8 us with both, from 1 tile per wave).
 // kCode: 0 a bf16 cache, 1 codes of e4m3, 2 codes of int8.
-// Codes take a ring of two tiles where four waves of a SIMD hold it (e4m3, up to
-// two tiles per wave: bound by latency), else one tile at a time in three waves.
-// (us per call, ring / one tile: e4m3 16384 entries 7.5 / 7.8, 2097152 entries
-// 112 / 100; int8 65536 entries 10.5 / 9.4, 2097152 entries 116 / 106.)
-constexpr bool coded_ring(int tpw, int code) { return code == 1 && tpw <= 2; }
+// Codes take a ring of two tiles where four waves of a SIMD hold it and a wave has
+// one tile (e4m3: bound by latency), else one tile at a time in three waves.
+// (us per call, ring / one tile: e4m3 16384 entries 7.9 / 8.2, 65536 10.2 / 9.9,
+// 2097152 145 / 127; int8 16384 entries 8.2 / 8.4, 65536 11.3 / 10.0, 2097152 149 / 128.)
+constexpr bool coded_ring(int tpw, int code) { return code == 1 && tpw == 1; }
 template <int kMode, int TPW, int kCode = 0>
 __global__ __launch_bounds__(kDraftThreads, kCode && !coded_ring(TPW, kCode) ? 3 : 2) void draft_kernel(DraftArgs a) {
     const DItem it = decode_ditem(a.seq, blockIdx.x, a.n_kv_heads, a.chunk);

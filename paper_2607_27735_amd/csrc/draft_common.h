@@ -159,7 +159,7 @@ __device__ __forceinline__ void coded_logits(float scale_log2, const u32x4 (&qop
 // bf16 numbers, the second of what the first leaves (16 bits): one of 8 bits is
 // as coarse as a bf16 output and far coarser than an fp32 one, and bf16 has fp32's
 // range, so that scales may lie anywhere.  (us per call, one number / two: 16384
-// entries 7.7 / 7.9; 262144 of int8 18.8 / 18.4; 512512 31.1 / 29.7.)
+// entries 7.7 / 7.9; 262144 of int8 18.8 / 18.4; 512512 31.1 / 30.6.)
 // The reference is 12 above the row's largest logit, so that values near fp32's
 // largest (the append's for an infinity is 2^128) do not pass its range before the
 // row is divided by its sum.
