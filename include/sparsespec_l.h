@@ -546,7 +546,10 @@ typedef struct {
  *     served sequences, -1 for the others and for t from the last token up to
  *     max_tokens;
  *   - total_len[b] = ctx + new where served, else ctx: a caller sees there who
- *     was not;
+ *     was not.  Verify and draft take lengths from the host: where pages or slots
+ *     may run out, total_len has to be read back first, since over a sequence that
+ *     was not served they would read table entries that name no page of its own
+ *     (in bounds, but another's keys or none);
  *   - free_range_out = {free_range[0] + pages taken, free_range[1]}.
  * ssl_page_map_bounded is the same call with the length of the free list
  * (n_free_pages >= 0, SSL_ERR_SHAPE otherwise): pages that free_range claims past

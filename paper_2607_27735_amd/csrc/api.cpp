@@ -1165,9 +1165,16 @@ size_t coded_bytes(const VerifyPlan& plan) {
 // there it saves the second pass over K and a launch, over several rounds the
 // chunks, as short as for bf16 (the LDS holds as many probabilities) but read
 // in half the time, wait too long for each other.  (us, stream / two: 1 x 2000
-// keys, 28 rows 13 / 15; 16 x 2000, 40 rows 29 / 45; 4 x 8000, 40 rows 29 / 37;
-// 32000, 28 rows 26 / 26; 16 x 8000, 8 rows 55 / 68; 120000, 8 rows 53 / 63;
-// several rounds: 16 x 8000, 28 rows 86 / 74; 4 x 32000, 40 rows 117 / 85.)
+// keys, 28 rows 13 / 14; 16 x 2000, 40 rows 29 / 46; 4 x 8000, 40 rows 29 / 38;
+// 32000, 28 rows 27 / 27; 16 x 8000, 8 rows 54 / 69; 120000, 8 rows 53 / 63;
+// several rounds: 16 x 8000, 28 rows 85 / 74; 4 x 32000, 40 rows 115 / 82.)
+// It holds where more than 40 rows run as row blocks, which read K and V once
+// each: 64/8 heads, 56 rows, one round: 1 x 1000 keys 16 / 18, 1 x 8000 22 / 24, 1 x
+// 20000 30 / 34, 4 x 4000 27 / 36; several: 2 x 12000 48 / 39, 4 x 8000 51 / 47;
+// 64 rows the same.  48 rows 25 / 26, 30 / 30 and 27 / 31, but for one sequence of
+// 2000 or 4000 keys 17.1 / 16.6 and 19.6 / 17.3.  And a batch that is ragged enough
+// for its items to end far apart: 64 x 1000 to 8191 keys, 28 rows 192 / 223, which
+// the rule, counting chunks, gives to two sweeps.
 bool coded_stream_wins(const VerifyPlan& plan) {
     return plan.stream_slots <= (int64_t)device_cus() * stream_blocks_per_cu();
 }

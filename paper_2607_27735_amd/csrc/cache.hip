@@ -18,12 +18,12 @@ using cc::u32x2;
 // forms the sums for itself (at most kMapBatch sequences), which saves the
 // kernel boundary or the exchange that sharing them would take, and then writes
 // its part of the slots and of the new table entries.  Bound by the launch and
-// three dependent loads (lengths, table, slots): 3.9 us per call back to back
-// for 16 sequences of 8 tokens, as an empty kernel takes; 4.7 for 64 sequences
-// and 315000 tokens.
+// three dependent loads (lengths, table, slots): 4.1 to 4.9 us per call back to
+// back for 16 sequences of 2 to 8 tokens (an empty kernel takes 3.9; the kernel
+// alone 2.9), 4.6 to 5.3 for 64 sequences and 315000 tokens (5.1).
 // ---------------------------------------------------------------------------
-// (Slots per workgroup for 64 prompts of 263000 tokens: 2048 10.5 us, 1024 7.6,
-// 512 and 256 6.7 per call.)
+// (Slots per workgroup, the kernel alone for 64 sequences and 315000 tokens: 2048
+// 9.2 us, 1024 6.4, 512 and 256 5.1.)
 constexpr int kMapThreads = 256;
 constexpr int kMapTokens = 512;    // slots per workgroup
 constexpr int kMapFar = 1 << 30;   // sums saturate here; no capacity reaches it
@@ -170,8 +170,8 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
 // A wave codes the new rows of one block and head: they stay in its registers
 // between the maximum and the codes, so K and V are read once, with no LDS.
 // Bound by those reads and writes, 2 + 1 bytes per element: 73635 tokens of 8
-// heads, 453 MB, take 91.6 us (4.95 TB/s; a copy on the device reaches 5.14), 64
-// sequences of 8 tokens 5.4 us, one of 8 3.8 us, the launch.
+// heads, 453 MB, take 92.4 us (4.90 TB/s; a copy on the device reaches 5.14), 64
+// sequences of 2 to 8 tokens 5.3 us, one of 7 3.9 to 4.6, the launch.
 // ---------------------------------------------------------------------------
 constexpr int kAppendWaves = 4;
 constexpr int kAppendThreads = kAppendWaves * kWave;

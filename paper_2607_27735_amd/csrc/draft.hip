@@ -18,11 +18,11 @@
 // end at the newest drafted token and is read straight from the cache.
 //
 // Over a coded cache (kCode) the entries' rows are 8-bit codes, gathered with
-// their two scales each; the rest is the same.  16384 entries (4.4 MB) take 7.4
+// their two scales each; the rest is the same.  16384 entries (4.4 MB) take 7.9
 // us per call back to back, of which a launch alone is 3.9 and the rest the chain
-// of index, table, scale and row loads and the merge; 262144 of int8 (70 MB) 18.9,
-// 3.7 TB/s of gathered rows; 512512 of e4m3, one set per query head (138 MB), 31.1,
-// 4.4 TB/s.
+// of index, table, scale and row loads and the merge; 262144 of int8 (70 MB) 18.4,
+// 3.8 TB/s of gathered rows; 512512 of e4m3, one set per query head (138 MB), 30.6,
+// 4.5 TB/s.  A round's step takes as long (8.1, 18.2).
 //
 // The tile math (gather, MFMA layouts, online softmax) is in draft_common.h.
 #include "coded_common.h"

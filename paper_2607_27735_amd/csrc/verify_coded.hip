@@ -16,14 +16,19 @@
 //
 // Bound by the codes' stream: 256 bytes per key and KV head in the first
 // kernel, K's 128 again in the second, which finds part of them in the caches.
-// Four sequences of 65536 keys, 48 rows, e4m3: 90 us for the sweep's 545 MB (6.0
-// TB/s; two workgroups per CU, so that one decodes while the other's loads are
-// under way) and 50 for the scores, which fetch 294 MB, so that little of K is
-// still in a cache; a ragged batch of 8 (298632 keys, 12 to 40 rows, int8): 114
-// (5.4 TB/s) and 57.  The matrix cores are busy for 14 to 21 % of that, the
-// vector units for 40 to 50 %.  Where a call's chunks run in one round the
-// streaming kernel of verify_stream.hip takes it, which reads K once and needs no
-// second launch.
+// Four sequences of 65536 keys, 48 rows, e4m3: 145 us per call back to back, for
+// 541 MB that the sweep fetches (two workgroups per CU, so that one decodes while
+// the other's loads are under way) and 288 for the scores, so that little of K is
+// still in a cache: 5.7 TB/s over the call.  Traced, each launch on its own, the
+// sweep takes 106 us in the median of 60 launches and 92 at the least, the scores
+// 63 and 49.  A ragged batch of 8 (298632 keys, 12 to 40 rows, int8): 170 us, 621
+// and 322 MB, 5.5 TB/s; traced 120 (112) and 64 (59).  The matrix cores are busy for
+// 14 to 22 % of that, the vector units for 42 to 52 %.  Where a call's chunks run in
+// one round the streaming kernel of verify_stream.hip takes it, which reads K once
+// and needs no second launch.
+// More than 48 rows take four row tiles in one workgroup per CU, all sequences of
+// the call alike (4 x 65536 keys, 56 rows: 180 to 187 us); more than 64 run in row
+// blocks, each with both passes (128 rows: 376).
 #include <stddef.h>
 
 #include "coded_common.h"

@@ -47,8 +47,9 @@
 // A cache of 8-bit codes (kCode) takes the fp32 form: rows of half the bytes,
 // decoded in registers to bf16 (K) and fp16 (V), their scales applied to the
 // logits and to the weights (coded_common.h).  32768 keys, 28 rows, e4m3: 26.2
-// us for 68 MB; the sweep itself ends after 14 us (11 in the median), at 5 TB/s,
-// and the rest is the exchange of steps 2 to 5.  The same call as two sweeps: 26.5.
+// us for 68 MB, as two sweeps 27.2.  Traced, the kernel takes 27.0 us and a build of
+// it that ends with step 1 16.3: the exchange of steps 2 to 5 is the rest (4096
+// keys, 20 rows: 12.8 and 6.1).
 // Publication, tags, epochs and bounded waits are those of verify_fused.hip.
 // The waits end: workgroups are dispatched in index order, the chunks of a
 // group (of both blocks, where two are interleaved) are consecutive and at most
