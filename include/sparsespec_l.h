@@ -596,12 +596,14 @@ int ssl_page_map_bounded(int32_t batch, int32_t page_size, int32_t max_blocks, i
  *   new codes are x / s rounded to the nearest code (ties to even).
  * (So s does not shrink when drafted tokens are rejected and overwritten.)
  * Rows after the last new one are not touched.  Infinities count as the largest
- * bf16, NaN as 0.  n_tokens = 0 does nothing.  Scales in the cache must be
- * finite and >= 0; powers of two make a code's rounding the only one.  Errors: SSL_ERR_NULL; SSL_ERR_SHAPE for n_kv_heads < 1, n_tokens
- * < 0, a stride too short, or sizes of the cache (n_pages, page_size < 1,
- * page_size not a multiple of scale_block, code unknown); SSL_ERR_UNSUPPORTED
- * if scale_block is not 32, 64 or 128, n_kv_heads > 65536, n_tokens > 2^27 or the
- * pools pass their limits; SSL_ERR_ALIGN.
+ * bf16, NaN as 0 (in V they count so in verify and draft too; a key that large has
+ * logits past what those allow, and rows that see it have no defined output).
+ * n_tokens = 0 does nothing.  Scales in the cache must be finite and >= 0; powers
+ * of two make a code's rounding the only one.  Errors: SSL_ERR_NULL; SSL_ERR_SHAPE
+ * for n_kv_heads < 1, n_tokens < 0, a stride too short, or sizes of the cache
+ * (n_pages, page_size < 1, page_size not a multiple of scale_block, code unknown);
+ * SSL_ERR_UNSUPPORTED if scale_block is not 32, 64 or 128, n_kv_heads > 65536,
+ * n_tokens > 2^27 or the pools pass their limits; SSL_ERR_ALIGN.
  */
 int ssl_cache_append(const ssl_coded_cache *cache, int32_t n_kv_heads, int32_t n_tokens,
                      const void *k_new, const void *v_new, int64_t k_stride, int64_t v_stride,
@@ -609,8 +611,9 @@ int ssl_cache_append(const ssl_coded_cache *cache, int32_t n_kv_heads, int32_t n
 
 /*
  * Verify attention with importance scores over a coded cache: as
- * ssl_verify_attn_paged, with keys and values code * scale.  Logits (which must be
- * finite there) and probabilities are fp32; the value product uses the probabilities
+ * ssl_verify_attn_paged, with keys and values code * scale.  Logits (which must lie
+ * within +-10^7; a row's normalizer is off by 2^-23 of its largest) and probabilities
+ * are fp32; the value product uses the probabilities
  * times V's scale, rounded to fp16 relative to their row's largest (11 bits; below
  * 2^-31 of it they lose bits, then count as 0), and the codes, which fp16 holds
  * exactly.  V's scales may be any that the append writes, or that are finite and
@@ -654,9 +657,9 @@ int ssl_verify_attn_coded(const ssl_shape *shape, const ssl_params *params,
  * Draft attention, and a step of a draft round, over a coded cache: as
  * ssl_draft_attn_paged and ssl_draft_step_paged (fixed rows through idx), with
  * keys and values code * scale; the value product uses the probabilities times
- * V's scale, to 16 bits (two bf16 numbers).  V's scales as for verify.  Workspaces from ssl_draft_workspace and
- * ssl_draft_step_workspace.  Other errors as there, and those of the
- * cache's sizes as in ssl_cache_append.
+ * V's scale, to 16 bits (two bf16 numbers).  Logits must be finite; V's scales as
+ * for verify.  Workspaces from ssl_draft_workspace and ssl_draft_step_workspace.
+ * Other errors as there, and those of the cache's sizes as in ssl_cache_append.
  */
 int ssl_draft_attn_coded(const ssl_shape *shape, const ssl_params *params,
                          const int32_t *n_idx_host, const void *q_draft,

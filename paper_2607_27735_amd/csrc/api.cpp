@@ -1796,7 +1796,7 @@ int ssl_page_map_bounded(int32_t batch, int32_t page_size, int32_t max_blocks, i
                           {ctx_len, batch}, {new_len, batch}, {free_range, 2}, {free_pages, listed}};
     for (int i = 0; i < 5; ++i)
         for (int j = i + 1; j < 9; ++j) {
-            const char *x = static_cast<const char*>(spans[i].p), *y = static_cast<const char*>(spans[j].p);
+            const uintptr_t x = reinterpret_cast<uintptr_t>(spans[i].p), y = reinterpret_cast<uintptr_t>(spans[j].p);
             if (spans[i].n > 0 && spans[j].n > 0 && x < y + 4 * spans[j].n && y < x + 4 * spans[i].n) return SSL_ERR_SHAPE;
         }
     PageMapArgs a = {};

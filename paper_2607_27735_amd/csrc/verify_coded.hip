@@ -19,11 +19,11 @@
 // Four sequences of 65536 keys, 48 rows, e4m3: 145 us per call back to back, for
 // 541 MB that the sweep fetches (two workgroups per CU, so that one decodes while
 // the other's loads are under way) and 288 for the scores, so that little of K is
-// still in a cache: 5.7 TB/s over the call.  Traced, each launch on its own, the
-// sweep takes 106 us in the median of 60 launches and 92 at the least, the scores
-// 63 and 49.  A ragged batch of 8 (298632 keys, 12 to 40 rows, int8): 170 us, 621
-// and 322 MB, 5.5 TB/s; traced 120 (112) and 64 (59).  The matrix cores are busy for
-// 14 to 22 % of that, the vector units for 42 to 52 %.  Where a call's chunks run in
+// still in a cache: 5.7 TB/s over the call.  A ragged batch of 8 (298632 keys, 12 to
+// 40 rows, int8): 170 us, 621 and 322 MB, 5.5 TB/s.  (Traced, each launch on its own,
+// sweep and scores take about 104 and 62 us in the median of 60 launches, 91 and 50
+// at the least; ragged about 123 and 65, 112 and 58.)  The matrix cores are busy for
+// 13 to 22 % of that, the vector units for 41 to 53 %.  Where a call's chunks run in
 // one round the streaming kernel of verify_stream.hip takes it, which reads K once
 // and needs no second launch.
 // More than 48 rows take four row tiles in one workgroup per CU, all sequences of

@@ -128,3 +128,31 @@ def test_verify_masks_keys_whose_logits_scale_to_nothing(sm, code, mode):
     c.ks[c.table[1, 0], 0, 0], c.ks[c.table[1, 0], 1, 0] = 0.0, 2.0 ** -126
     q, _ = ref.bf16_normal(rng, 2, 6, 8, 128, scale=1.5)
     check_verify(c, q, [6, 6], MODES[mode], sm=sm)
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("top", [1e3, 1e5, 9.9e6])
+def test_verify_large_logits(top, code, mode):
+    """One key takes each row, whichever tile it is in, and V's scales around it differ
+    by 2^60.  A normalizer M + log2(L) is two roundings of 2^-24 |logit| log2(e) off, in
+    log2 units: 2^-23 |logit| of itself."""
+    rng = np.random.default_rng(9)
+    c = ref.Cache(rng, [700], 1, 64, 32, code)
+    c.k[c.table[0], 0] = 0
+    c.ks[c.table[0]] = 1.0
+    for t, x in ((3, 2), (130, -3), (333, 3), (600, 1)):          # whole multiples of the logit's unit
+        mag = {1: (0x38, 1), 2: (0x40, 2), 3: (0x44, 3)}[abs(x)][code == "int8"]
+        sign = 0 if x > 0 else (128 if code == "e4m3" else None)
+        c.k[c.table[0, t // 64], 0, t % 64, 0] = np.uint8(256 - mag) if sign is None else mag + sign
+    c.vs[c.table[0]] = 2.0 ** rng.integers(-30, 31, c.vs[c.table[0]].shape)
+    q = torch.zeros(1, 3, 4, 128, dtype=torch.bfloat16)
+    q[..., 0] = torch.tensor([1.0, -1.0, 0.5, -0.25]) * (top / 3 / SM)
+    cache, table = on_gpu(c)
+    out, sc = B.verify_attn_coded(q.cuda(), cache, table, 700, [700], [3], B.make_params(SM, out_fp32=True, verify_mode=MODES[mode]))
+    torch.cuda.synchronize()
+    want, oabs, sh = ref.verify(c, q.double().numpy(), [3], SM, 16)
+    bar, least = 2.0 ** -9 + 2.0 ** -23 * top, 2.0 ** -31 * oabs.max(-1, keepdims=True)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= bar * oabs + least)
+    s, sh = sc.double().cpu().numpy(), sh.reshape(1, 1, 4, -1).sum(2)
+    assert np.array_equal(sh > 1e-3, s > 1e-3) and np.allclose(s[sh > 1e-3], sh[sh > 1e-3], rtol=bar)
