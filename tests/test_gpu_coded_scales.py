@@ -156,3 +156,15 @@ def test_verify_large_logits(top, code, mode):
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= bar * oabs + least)
     s, sh = sc.double().cpu().numpy(), sh.reshape(1, 1, 4, -1).sum(2)
     assert np.array_equal(sh > 1e-3, s > 1e-3) and np.allclose(s[sh > 1e-3], sh[sh > 1e-3], rtol=bar)
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("positions", [3, 10, 12, 16, 23])
+def test_verify_scales_of_any_size_in_every_row_tile(positions, mode):
+    """12 to 92 rows per KV head: one to four row tiles, and row blocks."""
+    rng = np.random.default_rng(positions)
+    c = ref.Cache(rng, [500, 260], 2, 64, 32, "e4m3")
+    c.vs[...] = np.where(np.isnan(c.vs), c.vs, 2.0 ** rng.integers(-100, 101, c.vs.shape))
+    q, _ = ref.bf16_normal(rng, 2, positions, 8, 128, scale=1.5)
+    check_verify(c, q, [positions, 2], MODES[mode])
+    check_verify(c, q, [positions, positions], MODES[mode], out_fp32=False)
